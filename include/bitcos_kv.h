@@ -137,11 +137,14 @@ int bitcos_kv_append(const bitcos_kv_cache* cache, int32_t tokens, int32_t act_d
  * kv head h / (q_heads / kv_heads).  For query i of n with kv_len keys,
  *   position p = kv_len - n + i; visible keys j: j < kv_len; causal: j <= p;
  *   window > 0: j > p - window as well;
- *   s_j = scale * sum_d q[d] k_j[d],  m = max_j s_j,  l = sum_j e^(s_j - m),
+ *   s_j = scale * sum_d q[d] k_j[d] (int8: the key's scale multiplies the sum),
+ *   m = max_j s_j,  l = sum_j e^(s_j - m),
  *   out = sum_j e^(s_j - m) v_j / l   (bfloat16, strides {token, head}),
  *   lse = m + ln l                    (fp32 [tokens][q_heads], or NULL).
- * A query that sees no key gets out = 0 and lse = -infinity.  Keys and values
- * that a query does not see have no part in its result, whatever they hold.
+ * A query that sees no key gets out = 0 and lse = -infinity; one that sees
+ * keys, all with the score -infinity, out = NaN (0 / 0) and lse = -infinity.
+ * Keys and values that a query does not see have no part in its result,
+ * whatever they hold.
  * Scores, m, l and the sums over values are fp32; products are exact (bf16 or
  * int8 times bf16); the weights e^(s_j - m) are rounded to bfloat16 (to twice
  * its digits where few queries share a request's keys) before they multiply

@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_attn_chunk_kernel(
       const auto p = __builtin_amdgcn_permlane32_swap(as_uint(l), as_uint(l), false, false);
       l = as_float(p[0]) + as_float(p[1]);
     }
-    bool odd = false;
+    bool odd = on && nothing_seen(A, I, tok, m, 64 * (I.t0 + k0), 64 * (I.t0 + k1));
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll

@@ -341,11 +341,14 @@ paged_attn_decode_kernel(AttnArgs, Parts P, int most, int least_log2) {
     float* pml = P.ml + (static_cast<int64_t>(me) * 2 + slot) * P.rows * 2;
     bool odd = false;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = 16 * nt + c;
+      odd |= row < rows && nothing_seen(A, I, static_cast<int>(row * A.group_inv >> 16), m[nt], 32 * (I.t0 + k0), 32 * (I.t0 + k1));
 #pragma unroll
       for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int i = 0; i < 4; ++i) odd |= !__builtin_isfinite(acc[nt][o][i]);
+    }
     odd = __any(odd);
     if (odd) rows_again<Value, D>(A, P, I, me, slot, whole, 32 * (I.t0 + k0), 32 * (I.t0 + k1), 0, rows);
 #pragma unroll

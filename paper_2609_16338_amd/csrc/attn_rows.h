@@ -18,6 +18,10 @@ constexpr int kOwn = BITCOS_KV_MAX_DIM / 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The maximum of a row that sees keys, all of them with the score -infinity: its sums stay zero, and its result is 0 / 0.
+// A row that sees no key has the maximum -infinity, and gives zeros.
+constexpr float kLowest = -__FLT_MAX__;
+
 // Maximum (base 2), sum of weights, and the lane's sums over values.
 struct RowSums {
   float m, l, acc[kOwn];
@@ -60,7 +64,7 @@ __device__ __forceinline__ RowSums row_over_keys(const AttnArgs& A, int r, int64
       }
       s *= kLog2e;
     }
-    float top = on ? s : -INFINITY;
+    float top = on ? fmaxf(s, kLowest) : -INFINITY;
 #pragma unroll
     for (int o = 32; o >= 1; o /= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float m1 = fmaxf(R.m, top), ref = m1 == -INFINITY ? 0.0f : m1;
@@ -88,10 +92,10 @@ __device__ __forceinline__ RowSums row_over_keys(const AttnArgs& A, int r, int64
   return R;
 }
 
-// The result of a row whose keys are all in.  No key seen: nothing was added (l > 0 otherwise, or NaN).
+// The result of a row whose keys are all in.
 __device__ __forceinline__ void row_out(const AttnArgs& A, const RowSums& R, int64_t t, int64_t head) {
   const int lane = threadIdx.x & 63;
-  const bool none = R.m == -INFINITY && R.l == 0.0f;
+  const bool none = R.m == -INFINITY;
   __bf16* out = reinterpret_cast<__bf16*>(A.out) + t * A.os[0] + head * A.os[1];
 #pragma unroll
   for (int i = 0; i < kOwn; ++i)

@@ -117,11 +117,20 @@ __device__ __forceinline__ bf16x8 widen8(u32x2 v) {
   return o;
 }
 
+// Whether a row of the item's token `tok` that sees some of keys [from, to) ended with the maximum of none: all their
+// scores are -infinity, or their pages are none of the cache's.  Which of the two, rows_again finds out.
+__device__ __forceinline__ bool nothing_seen(const AttnArgs& A, const Item& I, int tok, float m, int from, int to) {
+  int lo, hi;
+  seen(A, I.s, I.first + tok, lo, hi);
+  return m == -INFINITY && min(hi, to) > max(lo, from);
+}
+
 // Infinite and NaN values (or scales): in the products a weight of zero (a row
 // that does not see the key) would make NaN of them, and a weight in two halves, of which
 // the lower may be zero or negative, NaN of an infinity.  Either leaves a sum
 // that is not finite, and stays; so the rows of an item whose sums end up so
-// are done again one by one, over the keys that each sees of keys [from, to).
+// (or that saw nothing but scores of -infinity, above) are done again one by
+// one, over the keys that each sees of keys [from, to).
 template <class T, int D>
 __device__ __forceinline__ void rows_again(const AttnArgs& A, const Parts& P, const Item& I, int me, int slot, bool whole, int from, int to,
                                            int row0, int row1) {
