@@ -406,7 +406,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_attn_chunk_kernel(
       const auto p = __builtin_amdgcn_permlane32_swap(as_uint(l), as_uint(l), false, false);
       l = as_float(p[0]) + as_float(p[1]);
     }
-    bool odd = on && nothing_seen(A, I, tok, m, 64 * (I.t0 + k0), 64 * (I.t0 + k1));
+    // The weights 2^(s mul - m) take the product s mul as it is, but m, one of these products, rounded: a factor on all of
+    // them that the division by their sum takes out again, at most 2^(2^-5) up to |m| = 2^20.  Where m is huge it drives
+    // them all to zero or infinity: beyond that bound rows are done again, with one rounding for both.
+    bool odd = on && (nothing_seen(A, I, tok, m, 64 * (I.t0 + k0), 64 * (I.t0 + k1)) || (m > -INFINITY && fabsf(m) > 0x1p20f));
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll

@@ -129,8 +129,8 @@ __device__ __forceinline__ bool nothing_seen(const AttnArgs& A, const Item& I, i
 // that does not see the key) would make NaN of them, and a weight in two halves, of which
 // the lower may be zero or negative, NaN of an infinity.  Either leaves a sum
 // that is not finite, and stays; so the rows of an item whose sums end up so
-// (or that saw nothing but scores of -infinity, above) are done again one by
-// one, over the keys that each sees of keys [from, to).
+// (or that saw nothing but scores of -infinity, above, or huge ones) are done
+// again one by one, over the keys that each sees of keys [from, to).
 template <class T, int D>
 __device__ __forceinline__ void rows_again(const AttnArgs& A, const Parts& P, const Item& I, int me, int slot, bool whole, int from, int to,
                                            int row0, int row1) {
