@@ -269,7 +269,8 @@ extern "C" int bitcos_kv_append(const bitcos_kv_cache* cache, int32_t tokens, in
     const bool f32 = act_dtype == BITCOS_ACT_F32, i8 = cache->dtype == BITCOS_KV_I8;
     const auto fn = dim == 64 ? vector_kernel<64>(f32, i8) : dim == 128 ? vector_kernel<128>(f32, i8) : vector_kernel<256>(f32, i8);
     const int64_t per = 256 * 2 * (16 / in) / dim, blocks = (rows + per - 1) / per;
-    if (blocks <= INT32_MAX) {
+    // A launch holds fewer than 2^32 threads: one of more fails, or starts with the count's low 32 bits, with no error.
+    if (blocks * 256 <= UINT32_MAX) {
       hipLaunchKernelGGL(fn, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, static_cast<hipStream_t>(stream), A);
       return bitcos_launch_status();
     }
