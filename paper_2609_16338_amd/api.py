@@ -195,10 +195,17 @@ def bitcos_pack_device_noalloc(w_dev, scales_dev, dst_dev, group: int = 128, uni
 _GEMV = {FMT_BITCOS: "bitcos_gemv", FMT_TRIT5: "trit5_gemv", FMT_BIT2: "bit2_gemv"}
 
 
-def _stream_handle(stream):
+def _stream_handle(stream, dev=None):
     """The hipStream_t of `stream` (None: torch's current one) as an int.  The
     current stream's handle is read directly where torch offers it: building a
-    torch Stream object for it takes 3 us, as long as the launch itself."""
+    torch Stream object for it takes 3 us, as long as the launch itself.  With
+    `dev`, the GPU of the call's tensors, that has to be the current one, which
+    a launch goes to, and the stream's."""
+    if dev is not None:
+        if _t().cuda.current_device() != dev:
+            raise ValueError(f"the tensors are on cuda:{dev}, which is not the current device")
+        if getattr(stream, "device_index", dev) != dev:
+            raise ValueError(f"the tensors are on cuda:{dev}, the stream is not")
     if stream is not None:
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     torch = _t()
@@ -401,7 +408,7 @@ class KVCache:
             raise ValueError("a bfloat16 cache has no scales")
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device, self._dev = k.device, k.get_device()
         P = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self.desc = N.KVCacheDesc(N.KV_I8 if k.dtype == torch.int8 else N.KV_BF16, *k.shape, 0, k.stride()[:3], v.stride()[:3],
                                   k.data_ptr(), v.data_ptr(), P(k_scale), P(v_scale))
@@ -424,34 +431,37 @@ class StepPlan:
     cu_q int32 [requests + 1], kv_len int32 [requests], slots and positions int32 [max_tokens],
     ring_state int64 [2], counts int32 [4] (tokens, pages taken, pages given back, requests
     refused).  kv_len and ring_state are the next step's inputs, so an engine keeps two plans
-    and takes them in turn.  The tensors stay the ones made here."""
+    and takes them in turn.  The tensors stay the ones made here, on a GPU."""
 
     def __init__(self, requests: int, max_tokens: int, device="cuda"):
         torch = _t()
+        if torch.device(device).type != "cuda":
+            raise ValueError("a plan's tensors are written by a kernel: device must be a GPU")
         new = lambda n, dt=torch.int32: torch.zeros(n, dtype=dt, device=device)  # noqa: E731
         self.requests, self.max_tokens = requests, max_tokens
         self.cu_q, self.kv_len = new(requests + 1), new(requests)
         self.slots, self.positions = new(max_tokens), new(max_tokens)
         self.ring_state, self.counts = new(2, torch.int64), new(4)
+        self._dev = self.cu_q.get_device()
         self._out = tuple(t.data_ptr() for t in (self.cu_q, self.kv_len, self.slots, self.positions, self.ring_state, self.counts))
 
 
-def _i32(t, name, n=None):
-    """The address of a contiguous int32 cuda tensor of n elements (None: any number)."""
-    if t.dtype is not _torch.int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
-        raise ValueError(f"{name} must be a contiguous int32 cuda tensor" + ("" if n is None else f" of {n} elements"))
+def _i32(t, dev, name, n=None):
+    """The address of a contiguous int32 tensor on GPU `dev`, of n elements (None: any number)."""
+    if t.dtype is not _torch.int32 or t.get_device() != dev or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous int32 tensor on cuda:{dev}" + ("" if n is None else f" of {n} elements"))
     return t.data_ptr()
 
 
 _stride_arrays = {}  # strides {token, head, 1} -> the array that the C ABI takes
 
 
-def _rows(t, name, shape):
-    """The address and strides of a [tokens, heads, dim] cuda tensor, a head's values next to each other."""
+def _rows(t, dev, name, shape):
+    """The address and strides of a [tokens, heads, dim] tensor on GPU `dev`, a head's values next to each other."""
     st = t.stride()
     arr = _stride_arrays.get(st)
-    if t.shape != shape or not t.is_cuda or (arr is None and st[2] != 1):
-        raise ValueError(f"{name} must be a cuda tensor {list(shape)}, a head's values next to each other")
+    if t.shape != shape or t.get_device() != dev or (arr is None and st[2] != 1):
+        raise ValueError(f"{name} must be a tensor {list(shape)} on cuda:{dev}, a head's values next to each other")
     if arr is None:
         if len(_stride_arrays) > 1000:
             _stride_arrays.clear()
@@ -463,16 +473,16 @@ def kv_plan(kv_len, new_len, table, ring, ring_state, page_size: int, plan: Step
     """Enqueue the planning of a step on `stream`: pages, slots and positions of the new tokens
     (see bitcos_kv.h).  kv_len, new_len: int32 [requests]; table: int32 [requests, width]; ring:
     int32 [ring places]; ring_state: int64 [2]; `plan` receives the results, table and ring are
-    updated in place."""
+    updated in place.  All of them are on the plan's GPU, the current one."""
     torch = _t()
-    n = plan.requests
+    n, dev = plan.requests, plan._dev
     if table.dim() != 2 or table.shape[0] != n or ring.dim() != 1:
         raise ValueError("table must be [requests, width] and ring 1-D")
-    if ring_state.dtype is not torch.int64 or not ring_state.is_cuda or not ring_state.is_contiguous() or ring_state.numel() != 2:
-        raise ValueError("ring_state must be a contiguous int64 cuda tensor [2]")
-    st = N.lib().bitcos_kv_plan(_i32(kv_len, "kv_len", n), _i32(new_len, "new_len", n), n, _i32(table, "table"), table.shape[1],
-                                _i32(ring, "ring"), ring.numel(), ring_state.data_ptr(), page_size, plan.max_tokens, *plan._out,
-                                _stream_handle(stream))
+    if ring_state.dtype is not torch.int64 or ring_state.get_device() != dev or not ring_state.is_contiguous() or ring_state.numel() != 2:
+        raise ValueError(f"ring_state must be a contiguous int64 tensor [2] on cuda:{dev}")
+    st = N.lib().bitcos_kv_plan(_i32(kv_len, dev, "kv_len", n), _i32(new_len, dev, "new_len", n), n, _i32(table, dev, "table"),
+                                table.shape[1], _i32(ring, dev, "ring"), ring.numel(), ring_state.data_ptr(), page_size,
+                                plan.max_tokens, *plan._out, _stream_handle(stream, dev))
     if st:
         N.check(st, "bitcos_kv_plan")
     return plan
@@ -484,9 +494,10 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_out=None, rope=None, positi
 
     q, q_out: [tokens, q_heads, head_dim] of k's type and bfloat16: the queries as
     paged_attention reads them.  rope: None, or (cos, sin), contiguous float32 [positions,
-    rotated values / 2]; q and k are then rotated by positions (int32 [tokens or more])."""
+    rotated values / 2]; q and k are then rotated by positions (int32 [tokens or more]).  All
+    of them are on the cache's GPU, the current one."""
     torch = _t()
-    tokens = k.shape[0]
+    tokens, dev = k.shape[0], cache._dev
     dtype = k.dtype
     if dtype is torch.float32:
         act = N.ACT_F32
@@ -497,9 +508,9 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_out=None, rope=None, positi
     if v.dtype is not dtype or (q is not None and q.dtype is not dtype):
         raise TypeError("q, k and v must be of one type")
     shape = (tokens, cache.kv_heads, cache.head_dim)
-    kp, ks = _rows(k, "k", shape)
-    vp, vs = _rows(v, "v", shape)
-    at = _i32(slots, "slots")
+    kp, ks = _rows(k, dev, "k", shape)
+    vp, vs = _rows(v, dev, "v", shape)
+    at = _i32(slots, dev, "slots")
     if slots.numel() < tokens:
         raise ValueError("slots must have an entry for every token")
     hq = 0
@@ -509,21 +520,21 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_out=None, rope=None, positi
             raise ValueError("q must be [tokens, q_heads, head_dim]")
         hq = q.shape[1]
         shape = (tokens, hq, cache.head_dim)
-        qp, qs = _rows(q, "q", shape)
+        qp, qs = _rows(q, dev, "q", shape)
         if q_out is None or q_out.dtype is not torch.bfloat16:
             raise TypeError("q_out must be bfloat16")
-        op, os_ = _rows(q_out, "q_out", shape)
+        op, os_ = _rows(q_out, dev, "q_out", shape)
     rot = places = 0
     cp = sp = pp = None
     if rope is not None:
         cos, sin = rope
         angles = cos.shape
         if (len(angles) != 2 or sin.shape != angles or cos.dtype is not torch.float32 or sin.dtype is not torch.float32
-                or not (cos.is_cuda and sin.is_cuda and cos.is_contiguous() and sin.is_contiguous())):
-            raise ValueError("rope must be two contiguous float32 cuda tensors [positions, rotated values / 2]")
+                or cos.get_device() != dev or sin.get_device() != dev or not (cos.is_contiguous() and sin.is_contiguous())):
+            raise ValueError(f"rope must be two contiguous float32 tensors [positions, rotated values / 2] on cuda:{dev}")
         if positions is None:
             raise ValueError("rope needs positions")
-        pp = _i32(positions, "positions")
+        pp = _i32(positions, dev, "positions")
         if positions.numel() < tokens:
             raise ValueError("positions must have an entry for every token")
         places, rot = angles[0], 2 * angles[1]
@@ -531,7 +542,7 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_out=None, rope=None, positi
     if tokens == 0:
         return
     st = N.lib().bitcos_kv_append(cache._ref, tokens, act, kp, ks, vp, vs, at, hq, qp, qs, op, os_, rot, cp, sp, places, pp,
-                                  _stream_handle(stream))
+                                  _stream_handle(stream, dev))
     if st:
         N.check(st, "bitcos_kv_append")
 
@@ -553,33 +564,34 @@ def paged_attention(q, cache: KVCache, table, kv_len, cu_q, out, workspace, *, m
     [requests], the new tokens included; cu_q: int32 [requests + 1]; max_q, max_kv: what the host
     knows of the most new tokens and the most keys of a request; workspace: uint8 of
     paged_attention_workspace bytes; scale: 1 / sqrt(head_dim) unless given; window: keys that a
-    query sees at most (0: all); lse: None or float32 [tokens, q_heads]."""
+    query sees at most (0: all); lse: None or float32 [tokens, q_heads].  All of them are on the
+    cache's GPU, the current one."""
     torch = _t()
-    dim = cache.head_dim
+    dim, dev = cache.head_dim, cache._dev
     if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16:
         raise TypeError("q and out must be bfloat16")
     shape = q.shape
     if len(shape) != 3 or shape[2] != dim:
         raise ValueError("q must be [tokens, q_heads, head_dim]")
     tokens, hq, _ = shape
-    qp, qs = _rows(q, "q", shape)
-    op, os_ = _rows(out, "out", shape)
+    qp, qs = _rows(q, dev, "q", shape)
+    op, os_ = _rows(out, dev, "out", shape)
     if table.dim() != 2 or table.shape[0] < 1:
         raise ValueError("table must be [requests, width]")
     n, width = table.shape
-    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 cuda tensor")
+    if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
     lp = None
     if lse is not None:
-        if lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != shape[:2]:
-            raise ValueError("lse must be a contiguous float32 cuda tensor [tokens, q_heads]")
+        if lse.dtype is not torch.float32 or lse.get_device() != dev or not lse.is_contiguous() or lse.shape != shape[:2]:
+            raise ValueError(f"lse must be a contiguous float32 tensor [tokens, q_heads] on cuda:{dev}")
         lp = lse.data_ptr()
-    tp, kp, cp = _i32(table, "table"), _i32(kv_len, "kv_len", n), _i32(cu_q, "cu_q", n + 1)
+    tp, kp, cp = _i32(table, dev, "table"), _i32(kv_len, dev, "kv_len", n), _i32(cu_q, dev, "cu_q", n + 1)
     if tokens == 0:
         return out
     st = N.lib().bitcos_paged_attn(cache._ref, tokens, n, hq, qp, qs, tp, width, kp, cp, max_q, max_kv,
                                    1.0 / math.sqrt(dim) if scale is None else scale, causal, window, op, os_, lp,
-                                   workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+                                   workspace.data_ptr(), workspace.numel(), _stream_handle(stream, dev))
     if st:
         N.check(st, "bitcos_paged_attn")
     return out
