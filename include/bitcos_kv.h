@@ -161,8 +161,9 @@ int bitcos_kv_append(const bitcos_kv_cache* cache, int32_t tokens, int32_t act_d
  * Alignment: q, out and the cache 2 bytes (int8: 1); the matrix-core kernels
  * take heads of 64 and 128 values in pages of 16, 32, 64, ... tokens with up
  * to 128 query heads on a kv head, where everything lies on 16-byte boundaries
- * and a page spans less than 4 GiB (a token 2^24 elements); a general, much
- * slower kernel takes everything else.  Where a sum is not finite (an infinite
+ * and a page spans less than 4 GiB (a token 2^24 elements), and tables whose
+ * rows hold up to 2^31 - 8193 tokens; a general, much slower kernel takes
+ * everything else.  Where a sum is not finite (an infinite
  * or NaN key, value or scale within a request), its rows are done again one by
  * one, which takes many times as long.
  * Errors: E_ARG (null pointer, bad size; q_heads not a multiple of kv_heads;

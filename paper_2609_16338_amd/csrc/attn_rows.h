@@ -37,11 +37,12 @@ __device__ __forceinline__ RowSums row_over_keys(const AttnArgs& A, int r, int64
   RowSums R{-INFINITY, 0.0f, {}};
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) qv[i] = lane + 64 * i < dim ? static_cast<float>(q[lane + 64 * i]) : 0.0f;
-  for (int j0 = lo; j0 < hi; j0 += 64) {
-    const int j = j0 + lane;
-    bool on = j < hi;
+  for (int64_t j0 = lo; j0 < hi; j0 += 64) {  // (64 keys past the last may be past 2^31)
+    const int n = static_cast<int>(min(static_cast<int64_t>(64), hi - j0));
+    bool on = lane < n;
     int page = -1, off = 0;
     if (on) {
+      const int j = static_cast<int>(j0) + lane;
       const int p = j / A.c.page_size;
       off = j - p * A.c.page_size;
       page = A.table[static_cast<int64_t>(r) * A.width + p];
@@ -78,7 +79,6 @@ __device__ __forceinline__ RowSums row_over_keys(const AttnArgs& A, int r, int64
     p *= vs;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) R.acc[i] *= keep;
-    const int n = min(64, hi - j0);
     for (int x = 0; x < n; ++x) {
       if (!__builtin_amdgcn_readlane(on, x)) continue;
       const int64_t pg = __builtin_amdgcn_readlane(page, x), o = __builtin_amdgcn_readlane(off, x);

@@ -105,7 +105,9 @@ extern "C" int bitcos_paged_attn(const bitcos_kv_cache* cache, int32_t tokens, i
   A.scale = scale;
   // The schedule divides units (at most these) in doubles.
   const bool countable = (static_cast<double>(tokens) + requests) * cache->kv_heads * (A.kv_max / 32.0 + 2) < 1099511627776.0;
-  if (p.matrix && countable && rows_aligned16(q, q_stride, 2, 2) && rows_aligned16(out, out_stride, 2, 2)) {
+  // The matrix-core kernels form the numbers of up to 64 tiles of keys past the last in 32 bits.
+  const bool numbered = A.kv_max <= INT32_MAX - 8192;
+  if (p.matrix && countable && numbered && rows_aligned16(q, q_stride, 2, 2) && rows_aligned16(out, out_stride, 2, 2)) {
     A.tt = p.tt;
     A.tt_inv = ~uint64_t{0} / static_cast<uint64_t>(p.tt) + 1;
     A.group_inv = (65536 + A.group - 1) / A.group;
