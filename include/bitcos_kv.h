@@ -157,7 +157,9 @@ int bitcos_kv_append(const bitcos_kv_cache* cache, int32_t tokens, int32_t act_d
  *     that may overlap in time.
  *   - kv_len is read as at most table_width * page_size, cu_q as at most
  *     tokens; a key in a page whose id is outside [0, pages) is not visible.
- *     Rows of out and lse that belong to no request are left as they are.
+ *     Rows of out and lse that belong to no request are left as they are; where
+ *     cu_q does not ascend, a row that several requests name holds a mixture of
+ *     theirs or what it held.
  * Alignment: q, out and the cache 2 bytes (int8: 1); the matrix-core kernels
  * take heads of 64 and 128 values in pages of 16, 32, 64, ... tokens with up
  * to 128 query heads on a kv head, where everything lies on 16-byte boundaries

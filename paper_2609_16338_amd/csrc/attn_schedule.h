@@ -44,7 +44,7 @@ struct Item {
 
 template <int kTile>
 struct Schedule {
-  int64_t total = 0;  // units of all items (below 2^40: the host sees to it)
+  int64_t total = 0;  // units of all items (below 2^40: the host sees to it, for requests that share no token)
   int workers = 0;    // that share them
 
   static __device__ __forceinline__ int tiles_of(const AttnArgs& A, int n) {
@@ -145,6 +145,7 @@ struct Schedule {
       const int64_t here = lane_value(incl, 63);
       if (!place) {
         total += here;
+        if (total >> 40) return false;  // cu_q that does not ascend: nothing is done, rather than numbers that wrap
         if (r0 + 64 < A.requests) {
           r0 += 64;
           continue;
