@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_attn_chunk_kernel(
     // (one read for every tile would be waited for in every tile); and for each quarter which tiles' ids name none.
     int ids = 0, ids_from = 0;
     uint64_t none[4];
+    bool named = false;  // a page of this worker's tiles is one of the cache's
     const auto read_ids = [&](int kt) {
       const AttnArgs& A = args_anew();
       const int32_t* trow = A.table + static_cast<int64_t>(I.r) * A.width;
@@ -123,6 +124,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_attn_chunk_kernel(
         const bool bad = all[x] < 0 || all[x] >= A.c.pages;
         const int key0 = 64 * (I.t0 + kt + lane) + 16 * x;
         none[x] = __ballot(bad && key0 < I.hi && key0 + 16 > I.lo);
+        named |= __any(!bad && kt + lane < k1);
         if (x == wave) ids = bad ? -1 : all[x];
       }
     };
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_attn_chunk_kernel(
     // The weights 2^(s mul - m) take the product s mul as it is, but m, one of these products, rounded: a factor on all of
     // them that the division by their sum takes out again, at most 2^(2^-5) up to |m| = 2^20.  Where m is huge it drives
     // them all to zero or infinity: beyond that bound rows are done again, with one rounding for both.
-    bool odd = on && (nothing_seen(A, I, tok, m, 64 * (I.t0 + k0), 64 * (I.t0 + k1)) || (m > -INFINITY && fabsf(m) > 0x1p20f));
+    bool odd = on && ((named && nothing_seen(A, I, tok, m, 64 * (I.t0 + k0), 64 * (I.t0 + k1))) || (m > -INFINITY && fabsf(m) > 0x1p20f));
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll

@@ -116,6 +116,7 @@ paged_attn_decode_kernel(AttnArgs, Parts P, int most, int least_log2) {
     // The page ids of 64 half tiles, a lane each (-1: names no page, or no query sees its keys), read together and waited
     // for here: one read for every tile would be waited for in every tile.
     int ids = 0, ids_from = 0;
+    bool named = false;  // a page of this worker's tiles is one of the cache's
     const auto read_ids = [&](int kt) {
       const AttnArgs& A = args_anew();
       const int32_t* trow = A.table + static_cast<int64_t>(I.r) * A.width;
@@ -124,6 +125,7 @@ paged_attn_decode_kernel(AttnArgs, Parts P, int most, int least_log2) {
       ids = key0 < I.hi && key0 + 16 > I.lo ? trow[key0 >> A.page_shift] : -1;
       wait_vmem_all();
       if (ids >= A.c.pages) ids = -1;
+      named |= __any(ids >= 0 && kt + lane / 2 < k1);
     };
     // Where the item's keys and values lie (kv head h of page 0), bytes from page to page, and of the scales.
     const char *kbase, *vbase, *ksbase, *vsbase;
@@ -343,7 +345,7 @@ paged_attn_decode_kernel(AttnArgs, Parts P, int most, int least_log2) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int row = 16 * nt + c;
-      odd |= row < rows && nothing_seen(A, I, static_cast<int>(row * A.group_inv >> 16), m[nt], 32 * (I.t0 + k0), 32 * (I.t0 + k1));
+      odd |= named && row < rows && nothing_seen(A, I, static_cast<int>(row * A.group_inv >> 16), m[nt], 32 * (I.t0 + k0), 32 * (I.t0 + k1));
 #pragma unroll
       for (int o = 0; o < kOut; ++o)
 #pragma unroll

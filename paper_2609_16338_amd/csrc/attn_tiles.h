@@ -118,7 +118,8 @@ __device__ __forceinline__ bf16x8 widen8(u32x2 v) {
 }
 
 // Whether a row of the item's token `tok` that sees some of keys [from, to) ended with the maximum of none: all their
-// scores are -infinity, or their pages are none of the cache's.  Which of the two, rows_again finds out.
+// scores are -infinity, or their pages are none of the cache's.  Which of the two, rows_again finds out (slowly: not asked
+// for tiles without a page of the cache's, which a table may have many of).
 __device__ __forceinline__ bool nothing_seen(const AttnArgs& A, const Item& I, int tok, float m, int from, int to) {
   int lo, hi;
   seen(A, I.s, I.first + tok, lo, hi);
