@@ -201,18 +201,18 @@ def _stream_handle(stream, dev=None):
     torch Stream object for it takes 3 us, as long as the launch itself.  With
     `dev`, the GPU of the call's tensors, that has to be the current one, which
     a launch goes to, and the stream's."""
-    if dev is not None:
-        if _t().cuda.current_device() != dev:
-            raise ValueError(f"the tensors are on cuda:{dev}, which is not the current device")
-        if getattr(stream, "device_index", dev) != dev:
-            raise ValueError(f"the tensors are on cuda:{dev}, the stream is not")
-    if stream is not None:
-        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     torch = _t()
+    if stream is not None:
+        if dev is not None and (torch.cuda.current_device() != dev or getattr(stream, "device_index", dev) != dev):
+            raise ValueError(f"the tensors are on cuda:{dev}, the current device or the stream's is another")
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    here = torch.cuda.current_device()
+    if dev is not None and here != dev:
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{here}")
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if raw is None:
         return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    return raw(here)
 
 
 def gemv(L: Layout, blob_dev, x, y, xscale=None, y_mode: int = Y_F32, stream=None):
