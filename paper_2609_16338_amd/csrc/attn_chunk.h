@@ -13,13 +13,23 @@
 // while scores become weights (799 us against 643 for the prompt below), and
 // 32-key tiles for three workgroups a CU spill (839 us).
 //
-// Measured, 128 values a head: a prompt of 8192 (32/8 heads, bfloat16) 640 us,
-// 860 TFLOP/s; 1000 queries after 30000 int8 keys (40/8 heads) 798 us, 784
-// TFLOP/s; a library product of 16384 x 16384 matrices reaches 1363 TFLOP/s.
-// The matrix cores are busy for 50% of the cycles; a wave issues for 45% of
-// its time, waits for its turn to issue for 36%, for data for 19%.  Without the
-// copies the prompt would take 535 us, without either product 446, without the
-// exponentials 580: no single part bounds it, their issue on one SIMD does.
+// Measured with its join, 128 values a head: a prompt of 8192 (32/8 heads,
+// bfloat16) 642 us, 857 TFLOP/s; 1000 queries after 30000 int8 keys (40/8 heads)
+// 806 to 818 us, 764 to 775 TFLOP/s (the first ten launches of a burst up to
+// 1070 us each, then 787 and the join's 19); a library product of 16384 x 16384
+// matrices reaches 1363 TFLOP/s.  The matrix cores are busy for 50% (int8: 37%)
+// of the cycles, vector instructions issue for 49% (61%): between them all of
+// the time, so the two hardly overlap, though a product leaves the vector unit
+// half its cycles.  A wave issues for 45% of its time, waits for its turn to
+// issue for 36%, for data for 19%.  Without the copies the prompt would take
+// 535 us, without either product 446, without the exponentials 580.
+//
+// Weights multiply the values as one bfloat16, which is off by up to 2^-8 of
+// each where the few-row kernel's two halves lose 2^-16: a whole output's error
+// is 0.0022 so, 0.0017 (the result's own rounding) with both.  The second
+// product would be half of this kernel's matrix work again; for requests
+// of few queries alone, beside a chunk, it fits the registers at bfloat16 and
+// spills 14 to 57 of them at int8.
 //
 // As for few rows, scores stand transposed (S^T = K Q^T, 32 keys x 32 rows an
 // MFMA): lane l has row l % 32's scores of keys 8 a + 4 h + b (h = l / 32, a =
@@ -50,7 +60,8 @@ struct ChunkTile {
   static constexpr int kBytes = kKeys * kRow;  // of a tile of keys, or of values
   // Chunk c + low (low within c's alignment) of row r stands at at(c, low) ^ f(r).  Of widened int8 values the eight lanes
   // that write at once hold chunks of one parity: two to a bank, but for the bit of c (128 values) or r (64) that goes into
-  // the lowest.  1000 queries over 30000 keys so 798 us, with conflicts 805; a prompt of 8192 of 64 values 370 and 373.
+  // the lowest.  (The conflicts cost no time that shows: 1000 queries over 30000 keys 787 us with and without them, 300
+  // launches each.)
   // Rows of bfloat16 come straight to LDS and need none of it (a prompt of 128 values 642 us with it, 637 without).
   __device__ static __forceinline__ int at(int c, int low) { return kI8 ? c ^ c >> 3 ^ low : c + low; }
   __device__ static __forceinline__ int fk(int r) { return kChunks == 16 ? r & 15 : ((r >> 1) & 7) ^ (kI8 ? r & 1 : 0); }

@@ -15,9 +15,9 @@
 // Measured with its join, 128 values a head: 64 requests of 100 to 16384 keys
 // (32/8 heads, bfloat16, 801 MB) 137 us, 5.9 TB/s; 32 of up to 131072 (int8,
 // 1.84 GB) 293 us, 6.3 TB/s; a plain streaming read reaches 6.1 TB/s here.  No
-// LDS bank conflict; the vector units issue for 13% (int8: 55%) of the cycles.
-// One sequence of 2000 keys: 11.6 us, of which 7 are this kernel (finding its
-// place, the page ids, one tile: three dependent trips to memory) and 4 the join.
+// LDS bank conflict; the vector units issue for 14% (int8: 53%) of the cycles.
+// One sequence of 2000 keys: 12.0 us, of which 7 are this kernel (finding its
+// place, the page ids, one tile: three dependent trips to memory) and 4.5 the join.
 //
 // Scores stand transposed, S^T = K Q^T (16 keys x 16 rows an MFMA): a lane then
 // holds one row's scores of keys 4g .. 4g + 3 (g = lane / 16), the row maximum

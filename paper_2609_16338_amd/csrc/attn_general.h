@@ -1,6 +1,8 @@
 // Attention for any head size, page size, stride and alignment: one wave per
 // (query, head), all its keys (attn_rows.h).  Bound by the latency of reads
-// that do not coalesce; it stands for shapes that are rare, not for speed.
+// that do not coalesce; it stands for shapes that are rare, not for speed (one
+// request of 2000 keys, 32/8 heads: of 128 values 19 us by the matrix cores, of
+// 96 975 here, of 256 1940; a prompt of 1000 52, 3170, 7870 us).
 #pragma once
 
 #include "attn_rows.h"

@@ -18,7 +18,7 @@ using namespace bitcos_attn;
 // waves for many (256 / 512 / 1024: a prompt of 8192 898 / 642 / 650 us, a chunk
 // beside 16 single tokens 64 / 58 / 67 us), three where a head has 64 values,
 // whose rows and tiles take half the registers and LDS (a prompt of 8192, 24/4
-// heads, two / three: bfloat16 317 / 300 us, int8 401 / 374 us).
+// heads, two / three: bfloat16 363 / 329 us, int8 420 / 399 us).
 constexpr int kWaves = 2048, kGroups = 512, kGroups64 = 768;
 
 int launch_general(const AttnArgs& A, hipStream_t stream) {
@@ -43,8 +43,12 @@ AttnPlan plan_of(const bitcos_kv_cache* c, int32_t tokens, int32_t requests, int
   if (4ll * c->kv_heads * c->page_size > UINT32_MAX) return p;
   if (group > 128) return p;
   const int64_t want = static_cast<int64_t>(std::min(max_q, tokens)) * group;
-  // Rows that a wave's registers hold.  (24 requests of 5 tokens, 30 rows of 64 values: 21.4 us, in the other kernel 26.9.
-  // Single tokens beside a chunk go to the other kernel with it: launches of their own took 70 us where the mixture takes 58.)
+  // Rows that a wave's registers hold.  Drafted tokens, 24 requests of 30 to 6000 keys / 64 of 30 to 16000, here and in the
+  // other kernel, us: 128 values, 30 rows, bfloat16 70 / 320 and 67 / 336, int8 56 / 211 and 58 / 264; 5 rows 54 / 286 and
+  // 58 / 323, int8 39 / 166 and 55 / 263; 40 rows, which would spill here, 127 / 506 and 69 / 345.  64 values, 30 rows,
+  // bfloat16 31 / 92 and 26 / 97, int8 32 / 79 and 29 / 83; 48 rows 39 / 104 and 29 / 103, int8 42 / 112 and 31 / 96: those
+  // stay here for their weights' digits, not for speed.
+  // (Single tokens beside a chunk go to the other kernel with it: launches of their own took 70 us where the mixture takes 57.)
   const int few = c->head_dim == 64 ? 64 : 32;
   p.tiles = want > few || group > few ? 0 : want <= 16 ? 1 : want <= 32 ? 2 : 4;
   p.tt = std::min((p.tiles ? 16 * p.tiles : 128) / group, max_q);
