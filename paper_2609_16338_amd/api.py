@@ -380,6 +380,9 @@ def _check_xscale(L, xscale, m):
 # Paged key/value cache (device)
 # ---------------------------------------------------------------------------
 
+_I32_MAX = 2**31 - 1  # a larger number would reach the C ABI's 32 bits as another one
+
+
 class KVCache:
     """A paged cache of one layer: views of the caller's device tensors.
 
@@ -407,6 +410,8 @@ class KVCache:
         elif any(s is not None for s in scales):
             raise ValueError("a bfloat16 cache has no scales")
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        if self.pages * self.page_size > _I32_MAX or self.kv_heads > _I32_MAX:
+            raise ValueError("a cache holds fewer than 2^31 slots")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device, self._dev = k.device, k.get_device()
         P = lambda t: None if t is None else t.data_ptr()  # noqa: E731
@@ -478,6 +483,8 @@ def kv_plan(kv_len, new_len, table, ring, ring_state, page_size: int, plan: Step
     n, dev = plan.requests, plan._dev
     if table.dim() != 2 or table.shape[0] != n or ring.dim() != 1:
         raise ValueError("table must be [requests, width] and ring 1-D")
+    if page_size > _I32_MAX:
+        raise ValueError("page_size must be below 2^31")
     if ring_state.dtype is not torch.int64 or ring_state.get_device() != dev or not ring_state.is_contiguous() or ring_state.numel() != 2:
         raise ValueError(f"ring_state must be a contiguous int64 tensor [2] on cuda:{dev}")
     st = N.lib().bitcos_kv_plan(_i32(kv_len, dev, "kv_len", n), _i32(new_len, dev, "new_len", n), n, _i32(table, dev, "table"),
@@ -549,6 +556,8 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_out=None, rope=None, positi
 
 def paged_attention_workspace(cache: KVCache, tokens: int, requests: int, q_heads: int, max_q: int, max_kv: int) -> int:
     """Bytes of the workspace that paged_attention needs for these counts."""
+    if max(tokens, requests, q_heads, max_q, max_kv) > _I32_MAX:
+        raise ValueError("counts must be below 2^31")
     n = N.lib().bitcos_paged_attn_workspace(cache._ref, tokens, requests, q_heads, max_q, max_kv)
     if n == 0:
         raise ValueError("counts must be positive, and the cache's heads of 8 to 256 values in steps of 8")
@@ -578,6 +587,8 @@ def paged_attention(q, cache: KVCache, table, kv_len, cu_q, out, workspace, *, m
     op, os_ = _rows(out, dev, "out", shape)
     if table.dim() != 2 or table.shape[0] < 1:
         raise ValueError("table must be [requests, width]")
+    if max_q > _I32_MAX or max_kv > _I32_MAX or window > _I32_MAX:
+        raise ValueError("max_q, max_kv and window must be below 2^31")
     n, width = table.shape
     if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
