@@ -13,10 +13,10 @@
 // while scores become weights (799 us against 643 for the prompt below), and
 // 32-key tiles for three workgroups a CU spill (839 us).
 //
-// Measured with its join, 128 values a head: a prompt of 8192 (32/8 heads,
-// bfloat16) 642 us, 857 TFLOP/s; 1000 queries after 30000 int8 keys (40/8 heads)
-// 806 to 818 us, 764 to 775 TFLOP/s (the first ten launches of a burst up to
-// 1070 us each, then 787 and the join's 19); a library product of 16384 x 16384
+// Measured with its join, 128 values a head, on two cards: a prompt of 8192
+// (32/8 heads, bfloat16) 642 and 662 us, 857 and 831 TFLOP/s; 1000 queries after
+// 30000 int8 keys (40/8 heads) 816 and 838 us, 766 and 746 TFLOP/s (the first ten
+// launches of a burst up to 1070 us each); a library product of 16384 x 16384
 // matrices reaches 1363 TFLOP/s.  The matrix cores are busy for 50% (int8: 37%)
 // of the cycles, vector instructions issue for 49% (61%): between them all of
 // the time, so the two hardly overlap, though a product leaves the vector unit
